@@ -81,7 +81,7 @@ class PagedCache:
             abi.kv_pages(self.pool[l, 0], self.pool[l, 1], self.scale[l, 0] if e4m3 else None,
                          self.scale[l, 1] if e4m3 else None) for l in range(L)])
         self._table_host = torch.full((max_seqs, self.max_pages), -1, dtype=torch.int32)
-        self.table = self._table_host.to(dev)
+        self.table = self._table_host.to(dev, copy=True)
         self.seq_lens = torch.zeros(max_seqs, dtype=torch.int32, device=dev)
         self.lens, self._held, self._free = [], [], []
         self.device = dev
@@ -91,26 +91,42 @@ class PagedCache:
         """Empty the cache and give it sequences with room for these many rows each (none cached yet)."""
         if len(lengths) > self._table_host.shape[0]:
             raise ValueError(f"{len(lengths)} sequences: the cache holds {self._table_host.shape[0]}")
+        self._short(lengths, [0] * len(lengths), self.n_pages)  # refused with the cache as it was
         self._free = list(range(self.n_pages - 1, -1, -1))
         self._table_host.fill_(-1)
         self.lens, self._held = [0] * len(lengths), [0] * len(lengths)
         self.seq_lens.zero_()
-        self._reserve(lengths)
+        self._hand_out(lengths)
+        self.table.copy_(self._table_host)
 
-    def _reserve(self, rows):
-        changed = []
+    def _short(self, rows, held, free):
+        """How many pages each sequence lacks for these rows beside the `held` ones; ValueError where its table or the
+        free pages do not hold them."""
+        short = []
         for i, r in enumerate(rows):
             need = -(-r // self.page_size)
             if need > self.max_pages:
                 raise ValueError(f"sequence {i}: {r} rows, the table holds {self.max_pages * self.page_size}")
-            if need - self._held[i] > len(self._free):
-                raise ValueError("no free pages left")
-            while self._held[i] < need:
+            short.append(max(0, need - held[i]))
+        if sum(short) > free:
+            raise ValueError(f"no free pages left: {sum(short)} wanted, {free} free")
+        return short
+
+    def _hand_out(self, rows):
+        """Pages for these rows, in the host's table: all of them, or (ValueError) none.  The sequences that got some."""
+        changed = []
+        for i, k in enumerate(self._short(rows, self._held, len(self._free))):
+            for _ in range(k):
                 self._table_host[i, self._held[i]] = self._free.pop()
                 self._held[i] += 1
+            if k:
                 changed.append(i)
+        return changed
+
+    def _reserve(self, rows):
+        changed = self._hand_out(rows)
         if changed:
-            lo, hi = min(changed), max(changed) + 1
+            lo, hi = changed[0], changed[-1] + 1
             self.table[lo:hi].copy_(self._table_host[lo:hi])
 
     def _set_lens(self, lens):

@@ -217,3 +217,46 @@ def test_paged_cache_bookkeeping():
         c._reserve([18, 64, 65])
     with pytest.raises(ValueError):
         PagedCache(W.TINY_DECODER, 1, 1, 16, dtype="int4", device="cpu")
+
+
+def _agree(c):
+    """The device's table is the host's, and every page is free or one sequence's."""
+    assert c.table.data_ptr() != c._table_host.data_ptr()
+    assert c.table.tolist() == c._table_host.tolist()
+    used = [p for row in c.table.tolist() for p in row if p >= 0]
+    assert sorted(used + c._free) == list(range(c.n_pages))
+    assert [sum(p >= 0 for p in row) for row in c.table.tolist()][:len(c._held)] == c._held
+
+
+def test_a_refused_reservation_changes_nothing():
+    """A start or a growth that does not fit leaves the cache as it was, and what fits afterwards reaches the device's table."""
+    from synth import workloads as W
+    from paper_2609_29029_gb300 import PagedCache
+    c = PagedCache(W.TINY_DECODER, n_pages=5, max_seqs=3, max_len=64, page_size=16, device="cpu")
+    c.start([1, 1])
+    _agree(c)
+    for rows in ([33, 64], [33, 65], [64, 33]):  # too few pages; past the table
+        before = c.table.tolist()
+        with pytest.raises(ValueError):
+            c._reserve(rows)
+        assert c.table.tolist() == before
+        _agree(c)
+    c._reserve([33, 20])
+    assert c._held == [3, 2]
+    _agree(c)
+    c = PagedCache(W.TINY_DECODER, n_pages=6, max_seqs=3, max_len=64, page_size=16, device="cpu")
+    c.start([16, 32])
+    c._set_lens([16, 32])
+    c.grow()
+    before, lens = c.table.tolist(), c.lens
+    for lengths in ([32, 9999], [64, 33], [1, 1, 1, 1]):
+        with pytest.raises(ValueError):
+            c.start(lengths)
+        assert c.table.tolist() == before and c.lens == lens and c.seq_lens.tolist() == [16, 32, 0]
+        _agree(c)
+    c.start([32, 64])
+    _agree(c)
+    c.start([0, 16])  # sequences without pages, and none: no entry of the last start stays
+    _agree(c)
+    c.start([])
+    _agree(c)
