@@ -7,6 +7,7 @@ GPU; the counts are read back only for reporting (read_counts).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 from dataclasses import dataclass
 
@@ -65,7 +66,8 @@ class PagedCache:
     page table, the lengths, and a list of free pages (kept on the host).
 
     dtype "f16", or "e4m3" (8 bits, with a power-of-two scale for each row and head).  `start` gives it sequences,
-    `load` their prefilled rows, and each decode step (ScenePipeline.decode_paged) one more row a sequence."""
+    `load` their prefilled rows, and each decode step (ScenePipeline.decode_paged) one more row a sequence.  Each of
+    them runs on the stream it is given (the current one otherwise), behind the work of the one before it."""
 
     def __init__(self, dec, n_pages, max_seqs, max_len, page_size=64, dtype="f16", device="cuda"):
         if dtype not in ("f16", "e4m3"):
@@ -85,9 +87,30 @@ class PagedCache:
         self.seq_lens = torch.zeros(max_seqs, dtype=torch.int32, device=dev)
         self.lens, self._held, self._free = [], [], []
         self.device = dev
+        self._stream = None  # the last operation's, and the end of its work
+        self._done = torch.cuda.Event() if dev.type == "cuda" else None
         self.start([])
 
-    def start(self, lengths):
+    @contextlib.contextmanager
+    def _on(self, stream=None):
+        """The stream of an operation: made the current one, and behind the last operation's work."""
+        if self.device.type != "cuda":
+            yield None
+            return
+        s = stream if stream is not None else torch.cuda.current_stream(self.device)
+        with torch.cuda.stream(s):
+            if self._stream is not None and s != self._stream:
+                s.wait_event(self._done)
+                for t in (self.pool, self.scale, self.table, self.seq_lens):
+                    if t is not None:
+                        t.record_stream(s)
+            self._stream = s
+            try:
+                yield s
+            finally:
+                self._done.record(s)
+
+    def start(self, lengths, stream=None):
         """Empty the cache and give it sequences with room for these many rows each (none cached yet)."""
         if len(lengths) > self._table_host.shape[0]:
             raise ValueError(f"{len(lengths)} sequences: the cache holds {self._table_host.shape[0]}")
@@ -95,9 +118,10 @@ class PagedCache:
         self._free = list(range(self.n_pages - 1, -1, -1))
         self._table_host.fill_(-1)
         self.lens, self._held = [0] * len(lengths), [0] * len(lengths)
-        self.seq_lens.zero_()
         self._hand_out(lengths)
-        self.table.copy_(self._table_host)
+        with self._on(stream):
+            self.seq_lens.zero_()
+            self.table.copy_(self._table_host)
 
     def _short(self, rows, held, free):
         """How many pages each sequence lacks for these rows beside the `held` ones; ValueError where its table or the
@@ -139,22 +163,23 @@ class PagedCache:
         n, d = len(lengths), self.dec.d
         if n != len(self.lens) or any(self.lens):
             raise ValueError(f"{n} sequences loaded into a cache that holds {self.lens}: start() it with them first")
-        s = stream if stream is not None else torch.cuda.current_stream()
-        with torch.cuda.stream(s):
+        with self._on(stream) as s:
             self._reserve(lengths)
             for l in range(self.dec.n_layers):
                 abi.kv_append(self.pages[l], kv[l, 0], d, kv[l, 1], d, abi.RIFT_F16, T, cu_seqlens, self.seq_lens, n,
                               self.table, self.max_pages, stream=s)
             self._set_lens(lengths)
 
-    def grow(self):
+    def grow(self, stream=None):
         """Room for one more row of every sequence."""
-        self._reserve([L + 1 for L in self.lens])
+        with self._on(stream):
+            self._reserve([L + 1 for L in self.lens])
 
-    def advance(self):
+    def advance(self, stream=None):
         """One row a sequence was written: the lengths of the next step."""
         self.lens = [L + 1 for L in self.lens]
-        self.seq_lens[:len(self.lens)] += 1
+        with self._on(stream):
+            self.seq_lens[:len(self.lens)] += 1
 
 
 @dataclass
@@ -347,8 +372,7 @@ class ScenePipeline:
         """One decode step of every sequence of a paged cache, which it extends: token_ids[i] appended to
         sequence i.  Call it once for each token of the answers."""
         n = len(cache.lens)
-        s = stream if stream is not None else torch.cuda.current_stream()
-        with torch.cuda.stream(s):
+        with cache._on(stream) as s:
             cache.grow()
             need = abi.decode_paged_workspace_bytes(self.model.struct, n)
             if need > getattr(self, "ws_paged_bytes", 0):
