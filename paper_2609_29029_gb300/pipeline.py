@@ -89,6 +89,7 @@ class PagedCache:
         self.device = dev
         self._stream = None  # the last operation's, and the end of its work
         self._done = torch.cuda.Event() if dev.type == "cuda" else None
+        self._ws = None  # of a decode step; the cache's own, as steps of two caches may overlap
         self.start([])
 
     @contextlib.contextmanager
@@ -101,7 +102,7 @@ class PagedCache:
         with torch.cuda.stream(s):
             if self._stream is not None and s != self._stream:
                 s.wait_event(self._done)
-                for t in (self.pool, self.scale, self.table, self.seq_lens):
+                for t in (self.pool, self.scale, self.table, self.seq_lens, self._ws):
                     if t is not None:
                         t.record_stream(s)
             self._stream = s
@@ -157,6 +158,11 @@ class PagedCache:
         self.lens = list(lens)
         if lens:
             self.seq_lens[:len(lens)].copy_(torch.tensor(lens, dtype=torch.int32))
+
+    def _workspace(self, need):
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self._ws
 
     def load(self, kv, T, cu_seqlens, lengths, stream=None):
         """The prefilled rows (rift_prefill_layers' kv_out, fp16 [n_layers, 2, T, d]) of sequences of these lengths."""
@@ -375,11 +381,8 @@ class ScenePipeline:
         with cache._on(stream) as s:
             cache.grow()
             need = abi.decode_paged_workspace_bytes(self.model.struct, n)
-            if need > getattr(self, "ws_paged_bytes", 0):
-                self.ws_paged = torch.empty(need, dtype=torch.uint8, device=self.device)
-                self.ws_paged_bytes = need
             abi.decode_step_paged(self.model.struct, cache.pages, cache.table, cache.max_pages, cache.seq_lens, n, token_ids,
-                                  embed, embed.shape[0], hidden_out, logits, self.ws_paged, need, s)
+                                  embed, embed.shape[0], hidden_out, logits, cache._workspace(need), need, s)
             cache.advance()
 
     def run_batch(self, queries, prefill=True, stream=None):

@@ -79,3 +79,40 @@ def test_operations_follow_each_other_across_streams(pipe, embed, cuda, riftlib)
     assert got[0][0].abs().sum() > 0
     for outs in got[1:]:
         assert torch.equal(outs[0], got[0][0]) and torch.equal(outs[1][:, :2], got[0][1][:, :2])
+
+
+def test_two_caches_are_decoded_on_two_streams(pipe, embed, cuda, riftlib):
+    """Steps of two caches of one pipeline, enqueued in turn on a stream each: what each gives alone."""
+    lens = [[90, 70, 33], [50, 81]]
+    loads = [_rows(L, 5 + i, cuda) for i, L in enumerate(lens)]
+    ids = [torch.tensor(x, dtype=torch.int32, device=cuda) for x in ([3, 9, 27], [40, 41])]
+    side = [torch.cuda.Stream() for _ in range(2)]
+    steps, alone, both = 5, [], []
+
+    def fresh():
+        caches = []
+        for L, (kv, cu) in zip(lens, loads):
+            c = _cache(riftlib, cuda, n_pages=24)
+            c.start(L)
+            c.load(kv, sum(L), cu, L)
+            caches.append(c)
+        outs = [torch.zeros(steps, len(L), DEC.d, dtype=torch.bfloat16, device=cuda) for L in lens]
+        torch.cuda.synchronize()
+        return caches, outs
+
+    caches, alone = fresh()
+    for c, out, x in zip(caches, alone, ids):
+        _answer(pipe, c, embed, x, steps, None, out)
+        torch.cuda.synchronize()
+    for _ in range(4):
+        caches, both = fresh()
+        assert caches[0]._workspace(1).data_ptr() != caches[1]._workspace(1).data_ptr()
+        for s in side:
+            _busy(s, cuda)  # the steps pile up behind it, and run beside each other
+        for k in range(steps):
+            for c, out, x, s in zip(caches, both, ids, side):
+                pipe.decode_paged(c, x, embed, out[k], stream=s)
+        torch.cuda.synchronize()
+        riftlib.sync_status()
+        for got, want in zip(both, alone):
+            assert torch.equal(got, want)
