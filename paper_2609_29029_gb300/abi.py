@@ -430,6 +430,8 @@ def decode_paged_workspace_bytes(model: Model, n_seq) -> int:
 def decode_step_paged(model: Model, cache, page_table, max_pages, seq_lens, n_seq, token_ids, embed, vocab_embed,
                       hidden_out, logits, ws, ws_bytes, stream=None):
     """rift_decode_step_paged; cache: a ctypes array of KvPages, one a layer."""
+    if len(cache) < model.n_layers:
+        raise ValueError(f"{len(cache)} layers of pages for a model of {model.n_layers}")
     _check(lib.rift_decode_step_paged(C.byref(model), cache, ptr(page_table), max_pages, ptr(seq_lens), n_seq,
                                       ptr(token_ids), ptr(embed), vocab_embed, ptr(hidden_out), ptr(logits), ptr(ws),
                                       ws_bytes, stream_handle(stream)), "rift_decode_step_paged")

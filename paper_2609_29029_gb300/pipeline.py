@@ -377,7 +377,9 @@ class ScenePipeline:
     def decode_paged(self, cache: PagedCache, token_ids, embed, hidden_out=None, logits=None, stream=None):
         """One decode step of every sequence of a paged cache, which it extends: token_ids[i] appended to
         sequence i.  Call it once for each token of the answers."""
-        n = len(cache.lens)
+        n, dec = len(cache.lens), self.model.dec
+        if (cache.dec.n_layers, cache.dec.n_heads, cache.dec.head_dim) != (dec.n_layers, dec.n_heads, dec.head_dim):
+            raise ValueError("the cache was made for a decoder of other layers or heads")
         with cache._on(stream) as s:
             cache.grow()
             need = abi.decode_paged_workspace_bytes(self.model.struct, n)

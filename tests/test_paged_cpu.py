@@ -260,3 +260,23 @@ def test_a_refused_reservation_changes_nothing():
     _agree(c)
     c.start([])
     _agree(c)
+
+
+def test_a_cache_of_another_model_is_refused(riftlib):
+    """Fewer layers of pages than the model has would be read past their end."""
+    from types import SimpleNamespace
+    from synth import workloads as W
+    from paper_2609_29029_gb300 import PagedCache, ScenePipeline
+    m = riftlib.Model()
+    m.n_layers = 2
+    with pytest.raises(ValueError):
+        riftlib.decode_step_paged(m, (riftlib.KvPages * 1)(pages(riftlib)), FAKE, 4, FAKE, 3, FAKE, FAKE, 50, FAKE, None, FAKE, 0, 0)
+    cache = PagedCache(W.TINY_DECODER, n_pages=4, max_seqs=2, max_len=32, page_size=16, device="cpu")
+    cache.start([16, 16])
+    cache._set_lens([16, 16])
+    d = W.TINY_DECODER
+    for other in (W.DecoderShape(d.n_layers + 1, d.d, d.n_heads, d.head_dim, d.ffn, d.vocab),
+                  W.DecoderShape(d.n_layers, 2 * d.d, 2 * d.n_heads, d.head_dim, d.ffn, d.vocab)):
+        with pytest.raises(ValueError, match="another|other"):
+            ScenePipeline.decode_paged(SimpleNamespace(model=SimpleNamespace(dec=other, struct=m)), cache, None, None)
+        assert cache.lens == [16, 16] and cache._held == [1, 1]  # nothing reserved for the refused step
