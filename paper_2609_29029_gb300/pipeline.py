@@ -67,7 +67,9 @@ class PagedCache:
 
     dtype "f16", or "e4m3" (8 bits, with a power-of-two scale for each row and head).  `start` gives it sequences,
     `load` their prefilled rows, and each decode step (ScenePipeline.decode_paged) one more row a sequence.  Each of
-    them runs on the stream it is given (the current one otherwise), behind the work of the one before it."""
+    them runs on the stream it is given (the current one otherwise), behind the work of the one before it.  Pages and
+    lengths are counted on the host, so none can be captured into a graph: capture abi.decode_step_paged, with the
+    pages reserved before (`start` with longer lengths) and the device's lengths advanced in the graph."""
 
     def __init__(self, dec, n_pages, max_seqs, max_len, page_size=64, dtype="f16", device="cuda"):
         if dtype not in ("f16", "e4m3"):
@@ -100,6 +102,8 @@ class PagedCache:
             return
         s = stream if stream is not None else torch.cuda.current_stream(self.device)
         with torch.cuda.stream(s):
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("a PagedCache counts on the host: capture abi.decode_step_paged instead")
             if self._stream is not None and s != self._stream:
                 s.wait_event(self._done)
                 for t in (self.pool, self.scale, self.table, self.seq_lens, self._ws):
@@ -116,11 +120,11 @@ class PagedCache:
         if len(lengths) > self._table_host.shape[0]:
             raise ValueError(f"{len(lengths)} sequences: the cache holds {self._table_host.shape[0]}")
         self._short(lengths, [0] * len(lengths), self.n_pages)  # refused with the cache as it was
-        self._free = list(range(self.n_pages - 1, -1, -1))
-        self._table_host.fill_(-1)
-        self.lens, self._held = [0] * len(lengths), [0] * len(lengths)
-        self._hand_out(lengths)
         with self._on(stream):
+            self._free = list(range(self.n_pages - 1, -1, -1))
+            self._table_host.fill_(-1)
+            self.lens, self._held = [0] * len(lengths), [0] * len(lengths)
+            self._hand_out(lengths)
             self.seq_lens.zero_()
             self.table.copy_(self._table_host)
 
@@ -183,8 +187,8 @@ class PagedCache:
 
     def advance(self, stream=None):
         """One row a sequence was written: the lengths of the next step."""
-        self.lens = [L + 1 for L in self.lens]
         with self._on(stream):
+            self.lens = [L + 1 for L in self.lens]
             self.seq_lens[:len(self.lens)] += 1
 
 

@@ -116,3 +116,24 @@ def test_two_caches_are_decoded_on_two_streams(pipe, embed, cuda, riftlib):
         riftlib.sync_status()
         for got, want in zip(both, alone):
             assert torch.equal(got, want)
+
+
+def test_a_capture_is_refused(pipe, embed, cuda, riftlib):
+    """A replayed step would leave the host's lengths and pages behind: refused, with the cache as it was."""
+    lens = [40, 15]
+    kv, cu = _rows(lens, 9, cuda)
+    ids = torch.tensor([3, 9], dtype=torch.int32, device=cuda)
+    cache = _cache(riftlib, cuda)
+    cache.start(lens)
+    cache.load(kv, sum(lens), cu, lens)
+    out = torch.zeros(2, 2, DEC.d, dtype=torch.bfloat16, device=cuda)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        out[1].zero_()
+        for call in (lambda: pipe.decode_paged(cache, ids, embed, out[0]), lambda: cache.start([1]), cache.grow, cache.advance):
+            with pytest.raises(RuntimeError, match="host"):
+                call()
+    assert cache.lens == lens and cache._held == [3, 1]
+    _answer(pipe, cache, embed, ids, 2, None, out)
+    riftlib.sync_status()
+    assert cache.seq_lens[:2].tolist() == cache.lens == [42, 17] and out[1].abs().sum() > 0
