@@ -126,7 +126,7 @@ class PagedCache:
             self.lens, self._held = [0] * len(lengths), [0] * len(lengths)
             self._hand_out(lengths)
             self.seq_lens.zero_()
-            self.table.copy_(self._table_host)
+            self._to_device(self.table, self._table_host)
 
     def _short(self, rows, held, free):
         """How many pages each sequence lacks for these rows beside the `held` ones; ValueError where its table or the
@@ -156,12 +156,16 @@ class PagedCache:
         changed = self._hand_out(rows)
         if changed:
             lo, hi = changed[0], changed[-1] + 1
-            self.table[lo:hi].copy_(self._table_host[lo:hi])
+            self._to_device(self.table[lo:hi], self._table_host[lo:hi])
+
+    def _to_device(self, dst, src):
+        """A copy that the host does not wait for (of a pinned copy: the host's table may change before it is made)."""
+        dst.copy_(src.pin_memory() if self._done else src, non_blocking=True)
 
     def _set_lens(self, lens):
         self.lens = list(lens)
         if lens:
-            self.seq_lens[:len(lens)].copy_(torch.tensor(lens, dtype=torch.int32))
+            self._to_device(self.seq_lens[:len(lens)], torch.tensor(lens, dtype=torch.int32))
 
     def _workspace(self, need):
         if self._ws is None or self._ws.numel() < need:

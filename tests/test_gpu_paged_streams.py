@@ -36,7 +36,7 @@ def _busy(stream, cuda):
     """Some milliseconds of work on a stream, so that what follows on it comes late."""
     with torch.cuda.stream(stream):
         a = torch.zeros(4096, 4096, dtype=torch.bfloat16, device=cuda)
-        for _ in range(100):
+        for _ in range(200):
             a = a @ a
 
 
@@ -137,3 +137,32 @@ def test_a_capture_is_refused(pipe, embed, cuda, riftlib):
     _answer(pipe, cache, embed, ids, 2, None, out)
     riftlib.sync_status()
     assert cache.seq_lens[:2].tolist() == cache.lens == [42, 17] and out[1].abs().sum() > 0
+
+
+def test_the_host_does_not_wait_where_pages_are_added(pipe, embed, cuda, riftlib):
+    """Steps that begin a page of a sequence are enqueued behind running work, with the table as it stands then."""
+    lens = [16, 32, 31]
+    kv, cu = _rows(lens, 11, cuda)
+    ids = torch.tensor([3, 9, 27], dtype=torch.int32, device=cuda)
+    got = []
+    for busy in (False, False, True):  # the first one also allocates what is kept
+        cache = _cache(riftlib, cuda)
+        cache.start(lens)
+        cache.load(kv, sum(lens), cu, lens)
+        out = torch.zeros(18, 3, DEC.d, dtype=torch.bfloat16, device=cuda)
+        torch.cuda.synchronize()
+        held = list(cache._held)
+        if busy:
+            _busy(torch.cuda.current_stream(), cuda)
+            ev = torch.cuda.Event()
+            ev.record()
+        _answer(pipe, cache, embed, ids, 2, None, out)
+        if busy:
+            assert cache._held == [2, 3, 3] and held == [1, 2, 2]
+            assert not ev.query(), "the host waited for the stream"
+        _answer(pipe, cache, embed, ids, 16, None, out[2:])  # another page each, behind the same work
+        torch.cuda.synchronize()
+        riftlib.sync_status()
+        assert cache.table.tolist() == cache._table_host.tolist()
+        got.append(out)
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
