@@ -41,6 +41,7 @@
 #include <type_traits>
 
 #include "kv_pages.cuh"
+#include "paged_list.cuh"
 #include "rift_internal.h"
 
 namespace rift {
@@ -211,30 +212,6 @@ struct Items {
   }
 };
 
-// a / b for a >= 0, b > 0.  Three cases by size, as a 64-bit division takes hundreds of cycles and a 32-bit one about a
-// hundred: quotients below 2^20 by fp32 (off by one at most, put right).
-// (Not inlined: a small call runs each instruction about once, and fetching them is most of its time.)
-__device__ __noinline__ long long divide(long long a, long long b) {
-  if (((a | b) >> 31) != 0) return a / b;
-  const int x = (int)a, y = (int)b;
-  const float f = __fdividef((float)x, (float)y);
-  if (f >= 1048576.f) return (uint32_t)x / (uint32_t)y;
-  int q = (int)f, r = x - q * y;
-  if (r < 0) --q;
-  else if (r >= y) ++q;
-  return q;
-}
-// n things cut into k shares, the first ones a thing larger.
-struct Shares {
-  long long each, more;
-  __device__ __forceinline__ Shares(long long n, int k) : each(divide(n, k)), more(n - each * k) {}
-  __device__ __forceinline__ long long begin(int i) const { return each * i + min((long long)i, more); }
-  __device__ __forceinline__ int owner(long long x) const {  // the share that holds thing x
-    const long long large = more * (each + 1);
-    return (int)(x < large ? divide(x, each + 1) : more + divide(x - large, each));
-  }
-};
-
 __device__ __forceinline__ uint16_t bits16(float v, int bf16) {
   return bf16 ? __bfloat16_as_ushort(__float2bfloat16_rn(v)) : __half_as_ushort(__float2half_rn(v));
 }
@@ -328,15 +305,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
   }
   W *= per_seq;
   const int c = blockIdx.x, G = gridDim.x;
-  auto sequence_at = [&](long long want, int m) {  // the last of m sequences with `want` tiles or fewer before it
-    int lo = 0, hi = m;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) / 2;
-      if (tiles_before[mid] <= want) lo = mid;
-      else hi = mid;
-    }
-    return lo;
-  };
+  auto tiles = [&](int i) { return tiles_of<KT>(len[i], A.window); };
 
   // ---- the CTA's tiles [c0, c1) of the list, and the warp's [u0, u1) of them
   const Shares ctas(W, G);
@@ -354,19 +323,17 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
 #pragma unroll 1
       for (int pass = 0; pass < 2; ++pass) {  // the item that holds tile x: the CTA's borders (a lane each), then u0
         const long long x = pass == 0 ? (lane & 1 ? c1 : c0) : u0;
-        const int i = sequence_at(divide(x, per_seq), A.n_seq), n = tiles_of<KT>(len[i], A.window);
-        const long long base = tiles_before[i] * per_seq;
-        const int hb = (int)divide(min(x, W - 1) - base, n);
+        const ListItem at = item_at(x, W, per_seq, tiles_before, A.n_seq, tiles);
         if (pass == 0) {
-          const long long to = x >= W || n > max((long long)(WHOLE_KEYS / KT), ctas.each / 8) ? x : base + (long long)hb * n;
+          const long long to = x >= W || at.n > max((long long)(WHOLE_KEYS / KT), ctas.each / 8) ? x : at.base;
           c0 = __shfl_sync(0xffffffffu, to, 0);
           c1 = __shfl_sync(0xffffffffu, to, 1);
           cut_for_warps();
         } else {
-          it.seq = i;
-          it.base = base + (long long)hb * n;
-          it.head = A.hblocks == 1 ? hb : hb / A.hblocks;
-          it.blk = hb - it.head * A.hblocks;
+          it.seq = at.seq;
+          it.base = at.base;
+          it.head = A.hblocks == 1 ? at.block : at.block / A.hblocks;
+          it.blk = at.block - it.head * A.hblocks;
         }
       }
     }
@@ -376,15 +343,13 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
     for (int s0 = 0; s0 < A.n_seq; s0 += SEQS) {
       __syncthreads();
       const int m = min(SEQS, A.n_seq - s0);
-      const long long sum = fill(s0), want = divide(u0, per_seq) - passed;
-      if (u0 < u1 && it.seq < 0 && want < sum) {
-        const int i = sequence_at(want, m);
-        it.seq = s0 + i;
-        it.base = (passed + tiles_before[i]) * per_seq;
-        const int hb = (int)divide(u0 - it.base, tiles_of<KT>(len[i], A.window));
-        it.base += (long long)hb * tiles_of<KT>(len[i], A.window);
-        it.head = hb / A.hblocks;
-        it.blk = hb % A.hblocks;
+      const long long sum = fill(s0), x = u0 - passed * per_seq;
+      if (u0 < u1 && it.seq < 0 && x < sum * per_seq) {
+        const ListItem at = item_at(x, sum * per_seq, per_seq, tiles_before, m, tiles);
+        it.seq = s0 + at.seq;
+        it.base = passed * per_seq + at.base;
+        it.head = at.block / A.hblocks;
+        it.blk = at.block % A.hblocks;
       }
       passed += sum;
     }
