@@ -69,8 +69,11 @@ constexpr int SEQS = 1024;       // sequences whose lengths and tile counts a CT
 constexpr int WHOLE_KEYS = 640;
 // Weights are 2^(LIFT + s - m) for a running reference m that moves only when a score passes it by more than SLACK
 // (a vote, instead of a reduction over the warp and a rescaling for every 16 keys): at most 2^15, which fp16 holds, and
-// fp16 keeps all of its 11 bits down to 2^-23 of the reference (2^-14 for weights of at most one).
-constexpr float LIFT = 9.f, SLACK = 6.f;
+// fp16 keeps all of its 11 bits down to 2^-23 of the reference (2^-14 for weights of at most one).  Beside a bf16 cache they
+// are at most one: bf16 needs no lift, and its values may be so large (2^113 and more) that one takes the sums past fp32.
+constexpr float SLACK = 6.f;
+template <int CK>
+constexpr float LIFT = CK == CK_BF16 ? -SLACK : 9.f;
 
 template <int HD, int CK, int NB>
 struct Shape {
@@ -217,7 +220,10 @@ __device__ __forceinline__ uint16_t bits16(float v, int bf16) {
 }
 constexpr float LN2 = 0.6931471805599453f;
 // What a weight's exponent counts from; no score above -inf yet: 0, whose weights are 2^-inf.
-__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m - LIFT; }
+template <int CK>
+__device__ __forceinline__ float reference(float m) {
+  return m == -INFINITY ? 0.f : m - LIFT<CK>;
+}
 
 // Counts one more of `parts` arrivals at an item, in two words of the workspace: whether it was the last.  word[0] holds
 // KEY above the count, and the last arrival leaves a count of zero behind it, so that every call but a workspace's
@@ -647,12 +653,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
               const float down = top == -INFINITY ? 1.f : ex2(m[b][e] - top);
               l[b][e] *= down;
               m[b][e] = top;
-              from[b][e] = reference(top);
+              from[b][e] = reference<CK>(top);
               float down_o = down;
               if (CK == CK_E4M3) {
                 down_o = topv == -INFINITY ? 1.f : ex2(mv[b][e] - topv);
                 mv[b][e] = topv;
-                from_v[b][e] = reference(topv);
+                from_v[b][e] = reference<CK>(topv);
               }
 #pragma unroll
               for (int i = 0; i < DT; ++i) {
@@ -752,9 +758,9 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
         for (int d = 4; d < 32; d <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], d);
         const int h = 8 * b + 2 * t + e;
         if (h >= hn) continue;
-        const float sum = l[b][e], M = reference(m[b][e]);
+        const float sum = l[b][e], M = reference<CK>(m[b][e]);
         // no key at all (bad pages, scores of -inf): zero; e4m3 outputs stand relative to their own reference
-        const float to_y = sum == 0.f ? 0.f : (CK == CK_E4M3 ? exp2f(reference(mv[b][e]) - M) : 1.f) / sum;
+        const float to_y = sum == 0.f ? 0.f : (CK == CK_E4M3 ? exp2f(reference<CK>(mv[b][e]) - M) : 1.f) / sum;
         const long long head = (long long)kvh * A.group + h0 + h;
         if (whole) {
           uint16_t* dst = static_cast<uint16_t*>(A.out) + it.seq * A.out_stride + head * HD;
