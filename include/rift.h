@@ -460,8 +460,9 @@ rift_status rift_attention_varlen(const void* qkv, int T, const int* cu_seqlens,
  *                      turns that pair j makes over orig_len positions: pairs that turn `high`
  *                      times or more keep their frequency, those below `low` are interpolated
  *                      (the "by parts" interpolation of arXiv 2309.00071)
- * c and s are right to A (2^-34 + p w_j 2^-52) before their rounding to fp32; each product and sum is a rounded fp32
- * operation, and the result is rounded once to the type.  The inverse call is the gradient: it
+ * w_j is evaluated in doubles: right to w_j (8 + |ln theta|) 2^-53 (PLAIN, LINEAR; PARTS as its formula takes that on).
+ * For the w_j so evaluated c and s are right to A (2^-34 + |p| 2^-62) before their rounding to fp32 (A of 1e-30 or
+ * more).  Each product and sum is a rounded fp32 operation, and the result is rounded once to the type.  The inverse call is the gradient: it
  * takes dL/dy to dL/dx (and undoes the forward call when the amplitude is 1).
  *   x          [T] rows of n_heads * head_dim elements (heads contiguous), x_stride elements apart; dt is
  *              RIFT_F32, RIFT_F16 or RIFT_BF16

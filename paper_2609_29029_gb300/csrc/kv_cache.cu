@@ -663,20 +663,11 @@ RopeAngles rope_angles(const rift_rope_spec& s, bool inverse) {
   R.amplitude = (float)s.amplitude;
   R.amplitude_rest = (float)(s.amplitude - R.amplitude);
   R.ok = 1;
-  // theta^(-2j / rot_dim) as a product of two powers, each rounded once: a call has 16 to 24 of them to take, not 64 to 128
-  double fine[8], coarse = 1.0;
-  for (int i = 0; i < 8; ++i) fine[i] = i == 0 ? 1.0 : std::pow(s.theta, -2.0 * i / s.rot_dim);
+  double w[RIFT_ROPE_MAX_HEAD_DIM / 2];
+  rope_frequencies(s, w);
   for (int j = 0; j < s.rot_dim / 2; ++j) {
-    if (j % 8 == 0 && j > 0) coarse = std::pow(s.theta, -2.0 * j / s.rot_dim);
-    double w = coarse * fine[j % 8];
-    if (s.scaling == RIFT_ROPE_LINEAR) w /= s.factor;
-    if (s.scaling == RIFT_ROPE_PARTS) {
-      const double turns = s.orig_len * w / 6.283185307179586;
-      const double g = std::min(1.0, std::max(0.0, (turns - s.low) / (s.high - s.low)));
-      w *= g + (1.0 - g) / s.factor;
-    }
-    if (!(w <= 2147483648.0)) R.ok = 0;
-    else R.turns[j] = turns_of(w);
+    if (!(w[j] <= 2147483648.0)) R.ok = 0;
+    else R.turns[j] = turns_of(w[j]);
   }
   return R;
 }

@@ -3,10 +3,13 @@
 // A GB300 SM retires about two double operations a cycle, and a rotation of few heads has more angles than
 // that hides (4,091 rows of 16 pairs: 14.5 us, 5.1 of them the bytes').  So the angle is taken as a fraction of a turn in
 // 64-bit fixed point: the host gives f = 2^64 w / 2 pi (mod 2^64), and p f mod 2^64 is the fraction at any int32
-// position p, exact but for f's own rounding, with its quadrant in the top bits.  What is left, |x| <= pi / 4,
+// position p, exact but for f's own rounding to the nearest (of which p takes p pi 2^-64, below p 2^-62, into the
+// angle), with its quadrant in the top bits.  What is left, |x| <= pi / 4,
 // goes through the Taylor polynomials of sine and cosine, whose leading steps run on unevaluated sums of two fp32
 // values (Dekker's and Knuth's error-free sum and product): about 100 fp32 operations, good to 2^-34.
 #pragma once
+
+#include <algorithm>
 
 #include "rift_common.cuh"
 
@@ -72,12 +75,32 @@ __host__ __device__ __forceinline__ float2 cos_sin_of_turns(uint64_t turns, Floa
   return make_float2((quadrant + 1) & 2 ? -cosine : cosine, quadrant & 2 ? -sine : sine);
 }
 
-// 2^64 w / 2 pi modulo 2^64 for 0 <= w <= 2^31 (host): w's product with 1 / 2 pi as an unevaluated sum of two doubles.
+// 2^64 w / 2 pi modulo 2^64 for 0 <= w <= 2^31 (host), to the nearest integer: w's product with 1 / 2 pi as an unevaluated
+// sum of two doubles, p + e.  Whole turns leave p, whole units of 2^-64 turns what is left of it (both exactly), and only
+// the rest, with e, is rounded.
 inline uint64_t turns_of(double w) {
   const double inv = 0.15915494309189535, rest = -9.839338337591243e-18;
   const double p = w * inv, e = (std::fma(w, inv, -p) + w * rest) * 0x1p64;
-  const double fraction = p - (double)(long long)p;
-  return (uint64_t)(fraction * 0x1p64) + (uint64_t)(long long)(e < 0 ? e - 0.5 : e + 0.5);
+  const double fraction = (p - std::floor(p)) * 0x1p64, units = std::floor(fraction);
+  return (uint64_t)units + (uint64_t)(long long)std::floor(e + (fraction - units) + 0.5);
+}
+
+// w_j of a rotation's pairs j < rot_dim / 2 (host).  theta^(-2j / rot_dim) is a product of two powers, each rounded once: a
+// call has 16 to 24 of them to take, not 64 to 128.  The exponents' rounding is |ln theta| 2^-53 of w together, the powers'
+// (an ulp each) and the product's 5 2^-53 more, the factor's one.
+inline void rope_frequencies(const rift_rope_spec& s, double* w) {
+  double fine[8], coarse = 1.0;
+  for (int i = 0; i < 8; ++i) fine[i] = i == 0 ? 1.0 : std::pow(s.theta, -2.0 * i / s.rot_dim);
+  for (int j = 0; j < s.rot_dim / 2; ++j) {
+    if (j % 8 == 0 && j > 0) coarse = std::pow(s.theta, -2.0 * j / s.rot_dim);
+    w[j] = coarse * fine[j % 8];
+    if (s.scaling == RIFT_ROPE_LINEAR) w[j] /= s.factor;
+    if (s.scaling == RIFT_ROPE_PARTS) {
+      const double turns = s.orig_len * w[j] / 6.283185307179586;
+      const double g = std::min(1.0, std::max(0.0, (turns - s.low) / (s.high - s.low)));
+      w[j] *= g + (1.0 - g) / s.factor;
+    }
+  }
 }
 
 }  // namespace rift
