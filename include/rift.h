@@ -527,7 +527,7 @@ typedef struct {
  *               position; rot_dim a multiple of 16.  The turned key is rounded to dt before it is stored, as
  *               rift_rope followed by this call without rope would
  *   q, q_out    NULL, or (with rope) T rows of n_q_heads * head_dim elements turned the same way into q_out (q
- *               itself with the same stride, or memory apart)
+ *               itself with the same stride, or memory apart; apart from k and v)
  * A 16-bit cache holds the value rounded to its type (infinite beyond its range).  An RIFT_E4M3
  * cache takes, for each row and head, the smallest power of two 2^(b - 127), b >= 1, that brings the largest
  * finite magnitude to 448 or below, and holds the e4m3 value nearest to each element over it (ties
@@ -544,8 +544,8 @@ rift_status rift_kv_append(const rift_kv_pages* cache, const void* k, long long 
  * start[i] + r - cu[i] of its sequence i (cu_seqlens, start, T, n_seq as above), in dt (RIFT_F32, RIFT_F16 or
  * RIFT_BF16; rounded once, infinite beyond the type's range).  Rows that cannot be addressed are zero; rows
  * outside [cu[0], cu[n_seq]) are left alone.
- *   k, v        out, T rows of n_kv_heads * head_dim elements (either may be NULL); 16-byte aligned, strides
- *               multiples of 16 bytes */
+ *   k, v        out, T rows of n_kv_heads * head_dim elements (either may be NULL), apart from each other; 16-byte
+ *               aligned, strides multiples of 16 bytes */
 rift_status rift_kv_gather(const rift_kv_pages* cache, int T, const int* cu_seqlens, const int* start, int n_seq,
                            const int* page_table, int max_pages, void* k, long long k_stride, void* v,
                            long long v_stride, rift_dtype dt, rift_stream_t stream);
@@ -555,7 +555,8 @@ rift_status rift_kv_gather(const rift_kv_pages* cache, int T, const int* cu_seql
  * new token's own row among them: rift_kv_append it first); query head h reads key head
  * h / (n_heads / n_kv_heads).
  *   q, out      [n_seq] rows of n_heads * head_dim elements, q_stride and out_stride apart; dt RIFT_F16 or
- *               RIFT_BF16, the cache's own type where that has 16 bits
+ *               RIFT_BF16, the cache's own type where that has 16 bits.  out: q itself with the same stride, or memory
+ *               apart from it
  *   seq_lens    int32 [n_seq]; 0: the row of out is zero (lse -inf).  A length below 0 or past the table sets
  *               RIFT_ERR_CAPACITY and counts as 0; keys on a page outside the pool are left out
  *   window      0, or the rows each query sees: the last `window` of them

@@ -544,17 +544,22 @@ static bool rows_ok(const void* p, long long stride, long long width, rift_dtype
   return p && aligned16(p) && stride >= width && stride <= 0x7fffffffLL && stride * type_size(dt) % 16 == 0;
 }
 
-// Whether n_rows rows at a and at b (of the same width and type) share no memory, or are the same rows.
-static bool apart_or_same(const void* a, long long a_stride, const void* b, long long b_stride, long long n_rows,
-                          long long width, rift_dtype dt) {
-  if (a == b) return a_stride == b_stride;
+// Whether n_rows rows of a_width elements at a and of b_width at b share no memory.
+static bool apart(const void* a, long long a_stride, long long a_width, const void* b, long long b_stride, long long b_width,
+                  long long n_rows, rift_dtype dt) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   const int size = type_size(dt);
-  if (x + ((n_rows - 1) * a_stride + width) * size <= y || y + ((n_rows - 1) * b_stride + width) * size <= x) return true;
+  if (x + ((n_rows - 1) * a_stride + a_width) * size <= y || y + ((n_rows - 1) * b_stride + b_width) * size <= x) return true;
   // slices of the same rows (columns of one buffer)
   if (a_stride != b_stride) return false;
   const uintptr_t pitch = a_stride * size, off = (x > y ? x - y : y - x) % pitch;
-  return off >= (uintptr_t)(width * size) && off + width * size <= pitch;
+  const long long low = x < y ? a_width : b_width, high = x < y ? b_width : a_width;
+  return off >= (uintptr_t)(low * size) && off + high * size <= pitch;
+}
+// ... or, of one width, are the same rows.
+static bool apart_or_same(const void* a, long long a_stride, const void* b, long long b_stride, long long n_rows,
+                          long long width, rift_dtype dt) {
+  return (a == b && a_stride == b_stride) || apart(a, a_stride, width, b, b_stride, width, n_rows, dt);
 }
 
 static bool positive(double x) { return std::isfinite(x) && x > 0.0; }
@@ -651,6 +656,8 @@ rift_status rift_kv_append(const rift_kv_pages* cache, const void* k, long long 
     const long long qw = (long long)n_q_heads * P.head_dim;
     if (!rows_ok(q, q_stride, qw, dt) || !rows_ok(q_out, q_out_stride, qw, dt)) return RIFT_ERR_INVALID;
     if (!apart_or_same(q, q_stride, q_out, q_out_stride, T, qw, dt)) return RIFT_ERR_INVALID;
+    if (!apart(q_out, q_out_stride, qw, k, k_stride, width, T, dt) || !apart(q_out, q_out_stride, qw, v, v_stride, width, T, dt))
+      return RIFT_ERR_INVALID;
   }
   if (rope && rope->rot_dim % 16 != 0) return RIFT_ERR_UNSUPPORTED;
   RopeAngles R;
@@ -679,6 +686,7 @@ rift_status rift_kv_gather(const rift_kv_pages* cache, int T, const int* cu_seql
   const long long width = (long long)P.n_kv * P.head_dim;
   if ((!k && !v) || (k && !rows_ok(k, k_stride, width, dt)) || (v && !rows_ok(v, v_stride, width, dt)))
     return RIFT_ERR_INVALID;
+  if (k && v && !apart(k, k_stride, width, v, v_stride, width, T, dt)) return RIFT_ERR_INVALID;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   g_paged_used = true;
   prof_begin(RIFT_PROF_PACK, st);
@@ -712,6 +720,7 @@ rift_status rift_attention_paged(const rift_kv_pages* cache, const void* q, rift
   if (!seq_lens || !page_table) return RIFT_ERR_INVALID;
   const long long width = (long long)n_heads * P.head_dim;
   if (!rows_ok(q, q_stride, width, dt) || !rows_ok(out, out_stride, width, dt)) return RIFT_ERR_INVALID;
+  if (!apart_or_same(q, q_stride, out, out_stride, n_seq, width, dt)) return RIFT_ERR_INVALID;
   if (!ws_ok(ws, ws_bytes, rift_attention_paged_workspace_bytes(n_seq, n_heads, P.n_kv, P.head_dim))) return RIFT_ERR_INVALID;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   g_paged_used = true;

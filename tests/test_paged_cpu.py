@@ -280,3 +280,34 @@ def test_a_cache_of_another_model_is_refused(riftlib):
         with pytest.raises(ValueError, match="another|other"):
             ScenePipeline.decode_paged(SimpleNamespace(model=SimpleNamespace(dec=other, struct=m)), cache, None, None)
         assert cache.lens == [16, 16] and cache._held == [1, 1]  # nothing reserved for the refused step
+
+
+def test_outputs_that_overlap_inputs_are_refused(riftlib):
+    """Rows written while others of them are read: turned queries over keys or values, attention over part of its
+    queries, keys read back over values.  (Refused before anything is launched.)"""
+    lib, INV, F16 = riftlib.lib, riftlib.RIFT_ERR_INVALID, riftlib.RIFT_F16
+    p, sp, T = pages(riftlib), spec(riftlib), 4
+    FAR, W = 0x900000, 1024  # rows of q | k | v: 2 x 256, 256, 256 elements
+
+    def append(q_out, stride, k=FAKE + 1024, v=FAKE + 1536):
+        return lib.rift_kv_append(C.byref(p), k, W, v, W, F16, T, None, FAKE, T, FAKE, 4, C.byref(sp), FAKE, W, 8, q_out, stride, 0)
+
+    for q_out, stride in ((FAKE + 1024, W), (FAKE + 512, W), (FAR, 512)):
+        for k, v in ((q_out, FAKE + 1536), (FAKE + 1024, q_out), (q_out + 512, FAKE + 1536), (FAKE + 1024, q_out + 1008)):
+            assert append(q_out, stride, k, v) == INV, (q_out, stride, k, v)
+    assert append(FAKE, 512) == INV
+
+    def gather(k, ks, v, vs):
+        return lib.rift_kv_gather(C.byref(p), T, None, FAKE, T, FAKE, 4, k, ks, v, vs, F16, 0)
+
+    for k, ks, v, vs in ((FAKE, 256, FAKE, 256), (FAKE, 256, FAKE + 512, 256), (FAKE, 512, FAKE + 496, 512), (FAKE, 512, FAKE + 512, 264)):
+        assert gather(k, ks, v, vs) == INV and gather(v, vs, k, ks) == INV, (k, ks, v, vs)
+
+    need = riftlib.attention_paged_workspace_bytes(3, 8, 4, 64)
+
+    def attention(q, qs, out, os):
+        return lib.rift_attention_paged(C.byref(p), q, F16, qs, 8, FAKE, 3, FAKE, 4, 0, 0.0, out, os, None, FAR, need, 0)
+
+    for q, qs, out, os in ((FAKE, 512, FAKE, 520), (FAKE, 512, FAKE + 1024, 512), (FAKE, 1024, FAKE + 16, 1024),
+                           (FAKE, 1024, FAKE + 2048 + 1040, 1024), (FAKE + 16, 512, FAKE, 512)):
+        assert attention(q, qs, out, os) == INV, (q, qs, out, os)
