@@ -496,7 +496,8 @@ rift_status rift_rope(const void* x, rift_dtype dt, int T, int n_heads, int head
  *               the pools of several layers may be slices of one allocation
  *   dtype       RIFT_F16, RIFT_BF16, or RIFT_E4M3 with a power-of-two scale for each row and head:
  *               k_scale, v_scale uint8 [n_pages][n_kv_heads][page_size], the byte b standing for
- *               2^(b - 127): an element is its e4m3 code times that (NULL for the 16-bit types)
+ *               2^(b - 127): an element is its e4m3 code times that (NULL for the 16-bit types).  b is 1 .. 247 in
+ *               every row that is read (rift_kv_append writes no other; 448 2^120 passes fp32's largest value)
  *   page_size   a power of two, 1 .. 1024;  head_dim 64 or 128
  * Pools are 16-byte aligned and the strides multiples of 16 bytes (row_stride and head_stride below 2^31
  * elements, page_stride at most 2^40); rows of a page must not overlap.  The last row lies less than 2^32 units from
