@@ -567,8 +567,9 @@ rift_status rift_kv_gather(const rift_kv_pages* cache, int T, const int* cu_seql
  *   ws          rift_attention_paged_workspace_bytes(n_seq, n_heads, n_kv_heads, head_dim) bytes, used until the
  *               call's work is done (two calls that may overlap need one each, two graphs that may replay at
  *               once too)
- * Scores, softmax and sums are fp32 (a score of -inf is no key at all); the softmax weights enter the product
- * with V as the sum of two 16-bit numbers (fp16; bf16 for RIFT_BF16 caches).  The cache's memory past a sequence's rows may hold anything.
+ * Scores, softmax and sums are fp32.  A score of -inf has a weight of zero: a key that counts for nothing, as long as
+ * its values are finite (zero times an infinity or NaN is NaN).  The softmax weights enter the product with V as the sum
+ * of two 16-bit numbers (fp16; bf16 for RIFT_BF16 caches).  The cache's memory past a sequence's rows may hold anything.
  * n_heads is a multiple of n_kv_heads (up to 16 query heads read a key head's rows at once; a larger group
  * reads them once for every 16).  q, out 16-byte aligned, strides multiples of 16 bytes. */
 size_t rift_attention_paged_workspace_bytes(int n_seq, int n_heads, int n_kv_heads, int head_dim);
