@@ -69,11 +69,12 @@ constexpr int SEQS = 1024;       // sequences whose lengths and tile counts a CT
 constexpr int WHOLE_KEYS = 640;
 // Weights are 2^(LIFT + s - m) for a running reference m that moves only when a score passes it by more than SLACK
 // (a vote, instead of a reduction over the warp and a rescaling for every 16 keys): at most 2^15, which fp16 holds, and
-// fp16 keeps all of its 11 bits down to 2^-23 of the reference (2^-14 for weights of at most one).  Beside a bf16 cache they
-// are at most one: bf16 needs no lift, and its values may be so large (2^113 and more) that one takes the sums past fp32.
-constexpr float SLACK = 6.f;
+// fp16 keeps all of its 11 bits down to 2^-23 of the reference (2^-14 for weights of at most one).  bf16 needs no lift, and its
+// values may be so large (2^113 and more) that it takes the sums past fp32: DOWN, a power of two, brings those weights, and
+// those that join parts, to one a key at most.
+constexpr float LIFT = 9.f, SLACK = 6.f;
 template <int CK>
-constexpr float LIFT = CK == CK_BF16 ? -SLACK : 9.f;
+constexpr float DOWN = CK == CK_BF16 ? 1.f / 32768.f : 1.f;
 
 template <int HD, int CK, int NB>
 struct Shape {
@@ -220,10 +221,7 @@ __device__ __forceinline__ uint16_t bits16(float v, int bf16) {
 }
 constexpr float LN2 = 0.6931471805599453f;
 // What a weight's exponent counts from; no score above -inf yet: 0, whose weights are 2^-inf.
-template <int CK>
-__device__ __forceinline__ float reference(float m) {
-  return m == -INFINITY ? 0.f : m - LIFT<CK>;
-}
+__device__ __forceinline__ float reference(float m) { return m == -INFINITY ? 0.f : m - LIFT; }
 
 // Counts one more of `parts` arrivals at an item, in two words of the workspace: whether it was the last.  word[0] holds
 // KEY above the count, and the last arrival leaves a count of zero behind it, so that every call but a workspace's
@@ -653,12 +651,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
               const float down = top == -INFINITY ? 1.f : ex2(m[b][e] - top);
               l[b][e] *= down;
               m[b][e] = top;
-              from[b][e] = reference<CK>(top);
+              from[b][e] = reference(top);
               float down_o = down;
               if (CK == CK_E4M3) {
                 down_o = topv == -INFINITY ? 1.f : ex2(mv[b][e] - topv);
                 mv[b][e] = topv;
-                from_v[b][e] = reference<CK>(topv);
+                from_v[b][e] = reference(topv);
               }
 #pragma unroll
               for (int i = 0; i < DT; ++i) {
@@ -679,7 +677,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
               const float v = s[b][2 * r + e];
               const float x = ex2(v - from[b][e]);
               l[b][e] += x;
-              w[e] = CK == CK_E4M3 ? ex2(v + ev[r] - from_v[b][e]) : x;
+              w[e] = CK == CK_E4M3 ? ex2(v + ev[r] - from_v[b][e]) : x * DOWN<CK>;
             }
             if (CK == CK_BF16) {
               const uint32_t hi = pack_bf16x2(w[0], w[1]);
@@ -758,9 +756,9 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
         for (int d = 4; d < 32; d <<= 1) l[b][e] += __shfl_xor_sync(0xffffffffu, l[b][e], d);
         const int h = 8 * b + 2 * t + e;
         if (h >= hn) continue;
-        const float sum = l[b][e], M = reference<CK>(m[b][e]);
+        const float sum = l[b][e], M = reference(m[b][e]);
         // no key at all (bad pages, scores of -inf): zero; e4m3 outputs stand relative to their own reference
-        const float to_y = sum == 0.f ? 0.f : (CK == CK_E4M3 ? exp2f(reference<CK>(mv[b][e]) - M) : 1.f) / sum;
+        const float to_y = sum == 0.f ? 0.f : (CK == CK_E4M3 ? exp2f(reference(mv[b][e]) - M) : 1.f / DOWN<CK>) / sum;
         const long long head = (long long)kvh * A.group + h0 + h;
         if (whole) {
           uint16_t* dst = static_cast<uint16_t*>(A.out) + it.seq * A.out_stride + head * HD;
@@ -820,7 +818,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
       if ((members >> j & 1u) && y.y != 0.f) M = fmaxf(M, y.x);
     }
     const float2 y = part_ml[i][h];
-    part_w[i][h] = y.y == 0.f ? 0.f : y.y * exp2f(y.x - M);
+    part_w[i][h] = y.y == 0.f ? 0.f : y.y * exp2f(y.x - M) * DOWN<CK>;
     run_m[i][h] = M;
   }
   if (tid >= THREADS - 2 && leads) {  // only the first run can have begun before the CTA's tiles, only the last go on
@@ -865,11 +863,12 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
       uint16_t* dst = static_cast<uint16_t*>(A.out) + p.seq * A.out_stride + head * HD + d;
       *reinterpret_cast<ushort4*>(dst) = make_ushort4(bits16(acc.x * inv, q_bf16), bits16(acc.y * inv, q_bf16),
                                                       bits16(acc.z * inv, q_bf16), bits16(acc.w * inv, q_bf16));
-      if (A.lse && d == 0) A.lse[(long long)p.seq * A.n_heads + head] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * LN2;
+      if (A.lse && d == 0)
+        A.lse[(long long)p.seq * A.n_heads + head] = sum == 0.f ? -INFINITY : (M + log2f(sum / DOWN<CK>)) * LN2;
     } else {
       const long long at = (2LL * c + (starts ? 1 : 0)) * S::HG + h;
       *reinterpret_cast<float4*>(A.cta_o + at * HD + d) = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-      if (d == 0) A.cta_ml[at] = make_float2(M, sum);
+      if (d == 0) A.cta_ml[at] = make_float2(M, sum / DOWN<CK>);
     }
   }
 
@@ -910,7 +909,7 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
       M = warp_max(M);
       for (int i = lane; i < n; i += 32) {
         if (n > 32) ml = __ldcg(A.cta_ml + at(i) + h);
-        const float w = ml.y == 0.f ? 0.f : ml.y * exp2f(ml.x - M);
+        const float w = ml.y == 0.f ? 0.f : ml.y * exp2f(ml.x - M) * DOWN<CK>;
         weight[i * S::HG + h] = w;
         sum += w;
       }
@@ -944,7 +943,8 @@ __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_con
       uint16_t* dst = static_cast<uint16_t*>(A.out) + p.seq * A.out_stride + head * HD + d;
       *reinterpret_cast<ushort4*>(dst) = make_ushort4(bits16(acc.x * inv, q_bf16), bits16(acc.y * inv, q_bf16),
                                                       bits16(acc.z * inv, q_bf16), bits16(acc.w * inv, q_bf16));
-      if (A.lse && d == 0) A.lse[(long long)p.seq * A.n_heads + head] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * LN2;
+      if (A.lse && d == 0)
+        A.lse[(long long)p.seq * A.n_heads + head] = sum == 0.f ? -INFINITY : (M + log2f(sum / DOWN<CK>)) * LN2;
     }
     __syncthreads();
   }
