@@ -258,39 +258,26 @@ struct Part {
 };
 constexpr int PARTS = 2 * WARPS;  // at most two a warp: one of an item that began before its tiles, one of an item that
                                   // goes on behind them
-// What a CTA holds in shared memory beside its rings.
-template <int HG, int KW>
-struct Fixed {
-  long long scan[33], before[SEQS + 1];
-  int lens[SEQS];
-  uint32_t masks[WARPS][STAGES][KW];
-  Part parts[PARTS];
-  float2 part_ml[PARTS][HG];  // references (log2 units) and sums
-  float part_w[PARTS][HG], run_m[PARTS][HG];
-  int run[PARTS];
-  Part cut[2];                // what goes on in other CTAs: the item that began before, the one that goes on behind
-  int last[2], span[2][2];    // whether this CTA brought the item's last part; its first and last CTA
-};
 
 template <int HD, int CK, int NB>
 __global__ void __launch_bounds__(THREADS, 1) paged_attn_kernel(const __grid_constant__ Args A) {
   using S = Shape<HD, CK, NB>;
   constexpr int KT = S::KT, CPR = S::CPR, MB = KT / 16, KW = KT > 32 ? KT / 32 : 1, DT = HD / 16, QW = HD / 8;
-  static_assert(S::SMEM + sizeof(Fixed<S::HG, KW>) <= 227 * 1024, "the shared memory of an SM");
   constexpr uint32_t WHOLE = KT >= 32 ? 0xffffffffu : (1u << KT) - 1;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ Fixed<S::HG, KW> fixed;
-  auto& scan = fixed.scan;
-  auto& before = fixed.before;
-  auto& lens = fixed.lens;
-  auto& masks = fixed.masks;
-  auto& parts = fixed.parts;
-  auto& part_ml = fixed.part_ml;
-  auto &part_w = fixed.part_w, &run_m = fixed.run_m;
-  auto& run = fixed.run;
-  auto& last = fixed.last;
-  auto& cut = fixed.cut;
-  auto& span = fixed.span;
+  __shared__ long long scan[33], before[SEQS + 1];
+  __shared__ int lens[SEQS];
+  __shared__ uint32_t masks[WARPS][STAGES][KW];
+  __shared__ Part parts[PARTS];
+  __shared__ float2 part_ml[PARTS][S::HG];  // references (log2 units) and sums
+  __shared__ float part_w[PARTS][S::HG], run_m[PARTS][S::HG];
+  __shared__ int run[PARTS];
+  __shared__ Part cut[2];  // what goes on in other CTAs: the item that began before, the one that goes on behind
+  __shared__ int last[2], span[2][2];  // whether this CTA brought the item's last part; its first and last CTA
+  static_assert(S::SMEM + sizeof(scan) + sizeof(before) + sizeof(lens) + sizeof(masks) + sizeof(parts) + sizeof(part_ml) +
+                        sizeof(part_w) + sizeof(run_m) + sizeof(run) + sizeof(cut) + sizeof(last) + sizeof(span) + 256 <=
+                    227 * 1024,
+                "the shared memory of an SM (256: the arrays' alignment)");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
   const int per_seq = A.P.n_kv * A.hblocks;
   const int q_bf16 = CK == CK_BF16 ? 1 : CK == CK_F16 ? 0 : A.q_bf16;
