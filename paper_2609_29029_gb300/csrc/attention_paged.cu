@@ -6,16 +6,19 @@
 // into rings of their own (cp.async: a lane addresses its key's row through the page table, so a page may
 // end anywhere in a tile), and compute on them while the next tiles arrive.
 //
-// The work is the list of all (sequence, key head, up to 8 NB query heads) items, cut into tiles of KT keys, and
-// every CTA, and every warp of it, takes the same number of consecutive tiles: sequences of any mix of lengths
-// load the SMs evenly, and no warp waits for another before its tiles are done.  A warp writes the items that it
+// The work is the list of all (sequence, key head, up to 8 NB query heads) items, cut into tiles of KT keys.  Every CTA
+// takes the same number of consecutive tiles, but that a border inside a short item moves to the item's start (WHOLE_KEYS),
+// and every warp the same share of its CTA's: sequences of any mix of lengths load the SMs about evenly, and no warp
+// waits for another before its tiles are done.  A warp writes the items that it
 // holds whole; the warps of a CTA join their parts of items, (reference, sum, output), at its end, and where an item is
 // cut between CTAs, the one that brings the last part to the workspace joins them all (in the parts' order,
 // whichever that is).
 //
 // Measured (device time): 16 sequences of 8,192 to 32,768 rows, 32 query heads over 8 of 128 in bf16, 179 us for 1.17 GB,
-// 97% of the measured copy rate; 131,072 rows in e4m3 58 us for 271 MB (69%; 524,288 rows 92%): beside the stream
-// there are 4 to 5 us before the first tile (lengths, pages and tiles, a DRAM latency each) and as many behind the last.
+// 97% of the measured copy rate; 131,072 rows in e4m3 58 us for 271 MB (69%; 524,288 rows 84%, in pages of heads of rows
+// 92%).  What does not grow with the rows is 12 us of the first and 13 to 16 of the second (lines through calls of four
+// sizes): 4 to 5 before the first tile (lengths, pages and tiles, a DRAM latency each), as many behind the last, the rest
+// not accounted for; what grows runs at 7.0 TB/s, and 6.1 or (heads of rows) 7.2: reads alone pass the rate of a copy.
 // 73 sequences of 131 to 635 rows, 32 heads in fp16, 66 us for 384 MB; one of 635 rows 9 us.  A ring of two tiles ahead
 // (128 KB an SM in flight) is what the rate takes; 16 KB tiles in four warps held the shorter sequences up (124 us for
 // the 73).
@@ -36,6 +39,10 @@
 //    keeps 11 bits whatever the other rows' scales are, beside l = sum 2^(s - m).
 //  - weights of 16 bits would add their own rounding to the output's (in fp16 as much again, in bf16 ten times it):
 //    they enter as the sum of two, at the price of a second product that the stream hides (no change in time).
+//  - the products' sums are the tensor cores' own, which cut off below fp32's last bit at each step.  Before its rounding a long
+//    bf16 output is off by some 10^-5: 0.33% of those of the 16 sequences are not the nearest value (0.06% of a plain fp32
+//    form's).  Each 16 keys summed apart and a third bf16 number bring that to 0.03%, for 1 to 2% of the time there, 4
+//    to 8% of short sequences' and up to 15% with 16 heads an item: not taken, beside a bf16 step of 0.4%.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -64,8 +71,13 @@ constexpr int MAX_CTAS = 160;    // one an SM
 constexpr int STAGES = 3;        // tiles of a warp's ring
 constexpr int SEQS = 1024;       // sequences whose lengths and tile counts a CTA holds at a time
 // Items of up to this many keys, or up to an eighth of a CTA's share of tiles, are not cut between CTAs.  Joining an
-// item's parts across CTAs takes 3 to 4 us behind the last tile; these keys of one item take a CTA about as long (32 heads
-// of 635 rows: 13.7 us cut over all SMs, 10.8 whole on 32 of them).
+// item's parts across CTAs takes 3 to 4 us behind the last tile, and an SM streams faster than its share of HBM while others
+// have nothing left.  Both sides were measured at 540 points (1 to 24 sequences of 100 to 640 rows, 1, 8 and 32 key heads; fp16
+// x 128, e4m3 x 64, bf16 x 128 in groups of 4): whole was never slower.  Cut and whole, us, fp16: one key head of 600 rows
+// 11.5 and 8.6; 32 heads of 600 rows of 1, 5 and 10 sequences 10.7 and 9.7, 18.1 and 17.2 (the busiest CTA then has 76
+// tiles for an even share of 40), 25.2 and 23.2.  Up to some 1,000 rows whole stays ahead at most points; at 2,500 rows of
+// one head it takes 19.4 for 16.7.  Past SEQS sequences the borders' items would take a pass over the lengths to find, and a
+// share holds several items in any case: borders stay where they fall.
 constexpr int WHOLE_KEYS = 640;
 // Weights are 2^(LIFT + s - m) for a running reference m that moves only when a score passes it by more than SLACK
 // (a vote, instead of a reduction over the warp and a rescaling for every 16 keys): at most 2^15, which fp16 holds, and

@@ -353,7 +353,8 @@ __global__ void __launch_bounds__(KV_THREADS) rope_pairs_kernel(const T* x, int 
 }
 
 // Rows of a CTA: 64 KB of them (16 elements an item, `size` bytes each), but not so many that the GPU has fewer than four
-// CTAs an SM to work on at once, and no more rows than the table holds.  Half and twice as much, us: rope of 23,819 rows
+// CTAs an SM to work on at once, and no more rows than the table holds.  (The items of rope_pairs_kernel are pairs: its CTAs
+// get an eighth of that.)  Half and twice as much, us: rope of 23,819 rows
 // 115, 115, 118 (32 KB, 64 KB, 128 KB); in fp32 40, 43, 46 (64, 128, 256); e4m3 read back 61, 59, 62; stored and read back
 // 157, 150, 148.
 int rows_of_cta(int n_rows, int per_row, int half, int size) {
